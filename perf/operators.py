@@ -280,11 +280,10 @@ def prepare(case, seed):
         plan = fcp.fcp_plan_blocks(lens, bs, int(c["mask"] == "causal"), c["coalesce"], owned)
     flags = fcp.FCP_FLAG_DIRECT_SINGLE
     if c["train"]:
-        # the backward's D = rowsum(dO o O) wants the O that has not been rounded; the projection behind the attention takes a bf16 copy
-        flags |= fcp.FCP_FLAG_O_F32 | fcp.FCP_FLAG_GRAD_BF16 | (fcp.FCP_FLAG_BWD_SPILL_DS if c["spill"] else 0)
+        flags |= fcp.FCP_FLAG_GRAD_BF16 | (fcp.FCP_FLAG_BWD_SPILL_DS if c["spill"] else 0)
         s.dq, s.dk, s.dv = empty(t_q, hq, d), empty(t_kv, hkv, d), empty(t_kv, hkv, d)
     s.problem = fcp.Problem(plan, hq, hkv, d, bs, 0.0, flags, softcap=c["cap"], slopes=_slopes(c))
-    s.o, s.lse = empty(t_q, hq, d, dtype=torch.float32 if c["train"] else torch.bfloat16), empty(t_q, hq, dtype=torch.float32)
+    s.o, s.lse = empty(t_q, hq, d), empty(t_q, hq, dtype=torch.float32)
     rows = max(1, s.problem.n_slot_rows)
     s.o_part, s.lse_part = empty(rows, hq, d, dtype=torch.float32), empty(rows, hq, dtype=torch.float32)
     n = fcp.fcp_workspace_bytes(s.problem)
@@ -308,9 +307,8 @@ def run(s):
     fcp.fcp_merge_partials(s.problem, s.o_part, s.lse_part, s.o, s.lse, s.ws_ptr, stream)
     if not s.case["train"]:
         return s.o, s.lse
-    out = s.o.to(torch.bfloat16)
     fcp.fcp_block_attn_bwd(s.problem, s.q, s.k, s.v, s.o, s.lse, s.d_o, s.dq, s.dk, s.dv, s.ws_ptr, stream)
-    return out, s.lse, s.dq, s.dk, s.dv
+    return s.o, s.lse, s.dq, s.dk, s.dv
 
 
 def _plain_rope(s):
