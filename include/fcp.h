@@ -103,7 +103,9 @@ enum {
   FCP_FLAG_SCORES = 128,         /* the descriptor's `scores` is there and says how scores are formed.  The slopes, and the positions that the
                                     tables imply, are copied by fcp_queue_build; softcap is read by every call (and the backward needs the
                                     forward's).  Set it before fcp_workspace_bytes / fcp_queue_build and keep it for every call on the
-                                    workspace.  Works with every other flag. */
+                                    workspace.  Works with every other flag.  A workspace built with slopes serves the same tables with plain and capped
+                                    scores too (layers of several kinds in turn); one built without them serves no slopes
+                                    (FCP_ERR_INVALID_ARG). */
   FCP_FLAG_DIRECT_SINGLE = 2     /* a query block with ONE slot needs no reduction: fcp_block_attn_fwd_out writes its
                                     result straight to the final o / lse and fcp_merge_partials leaves it alone.
                                     Set it before fcp_workspace_bytes / fcp_queue_build and keep it for every call

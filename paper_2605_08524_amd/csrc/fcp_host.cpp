@@ -500,7 +500,8 @@ int compute_layout(const fcp_problem* p, bool forward_only, WsLayout* L) {
   // last of the tables: there are usually far fewer spans than the layout has room for, and only those are uploaded (4142 pairs,
   // 257 spans, 16 heads: queue builder 406 us with all of the room, 387 so; forward without a workspace 163 and 151)
   L->off_spans = off;       off = align(off + sizeof(DevPair) * (size_t)std::max<int64_t>(1, L->n_spans));
-  // What a distance bias needs: behind the rest, so that plain and capped scores find their tables in a workspace built with slopes.
+  // What a distance bias needs: sections that a problem without slopes does not have.  On a workspace built with slopes plain and capped scores
+  // go by the layout that it was built with (layout_for), so that their scratch does not lie on these.
   L->bias = has_bias(p);
   L->off_slopes = off;      off = align(off + (L->bias ? sizeof(float) * (size_t)p->n_q_heads : 0));
   L->off_span_rel = off;    off = align(off + (L->bias ? sizeof(int32_t) * (size_t)std::max<int64_t>(1, L->n_spans) : 0));
@@ -744,7 +745,8 @@ void choose_split(const fcp_problem* p, bool forward_only, WsLayout* L) {
 // workspace with the same descriptor scalars reuses the layout instead of walking every table again: the
 // kernels read the device copy of the tables that fcp_queue_build made, so the host tables matter to a
 // launch only through their counts.  A workspace the registry does not know (or a descriptor that differs)
-// takes the full validation path.
+// takes the full validation path.  Scores are not part of the key: a workspace built with slopes serves all kinds, each by
+// the layout that it was built with; one built without them has none to read.
 namespace {
 struct LayoutKey {
   const void* workspace;
@@ -752,7 +754,7 @@ struct LayoutKey {
   bool operator==(const LayoutKey& o) const { return workspace == o.workspace && std::memcmp(v, o.v, sizeof(v)) == 0; }
 };
 LayoutKey make_key(const fcp_problem* p, const void* ws) {
-  return LayoutKey{ws, {p->n_q_heads, p->n_kv_heads, p->head_dim, p->block_size, (p->flags & (FCP_FLAG_DIRECT_SINGLE | FCP_FLAG_BWD_SPILL_DS | FCP_FLAG_WHOLE_ITEMS)) | (has_bias(p) ? FCP_FLAG_SCORES : 0),
+  return LayoutKey{ws, {p->n_q_heads, p->n_kv_heads, p->head_dim, p->block_size, p->flags & (FCP_FLAG_DIRECT_SINGLE | FCP_FLAG_BWD_SPILL_DS | FCP_FLAG_WHOLE_ITEMS),
                         p->n_kv_blocks, p->n_q_blocks, p->n_pairs, p->n_slots, p->n_slot_rows, p->n_segments}};
 }
 constexpr int kLayoutCacheSize = 32;
@@ -776,10 +778,10 @@ int layout_for(const fcp_problem* p, const void* workspace, WsLayout* L) {
     const LayoutKey key = make_key(p, workspace);
     std::lock_guard<std::mutex> lock(g_layout_mutex);
     for (int i = 0; i < g_layout_count; i++) {
-      if (g_layout_cache[i].first == key) { *L = g_layout_cache[i].second; return FCP_OK; }
       if (g_layout_cache[i].first.workspace == workspace && has_bias(p) && !g_layout_cache[i].second.bias) {
         set_error("scores: the workspace was built without slopes"); return FCP_ERR_INVALID_ARG;
       }
+      if (g_layout_cache[i].first == key) { *L = g_layout_cache[i].second; return FCP_OK; }
     }
   }
   try {

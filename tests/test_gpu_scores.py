@@ -482,3 +482,26 @@ def test_two_graphs_share_a_workspace(whole):
         graphs[cap].replay()
         for name, x in run.outputs().items():
             assert np.array_equal(x, eager[cap][name]), (cap, name)
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("spill", [0, fcp.FCP_FLAG_BWD_SPILL_DS], ids=["recompute", "spill"])
+@pytest.mark.parametrize("lens,d", [([300, 40], 64), ([700, 260], 128)])
+def test_layers_of_several_kinds_of_scores_take_turns_on_one_workspace(lens, d, spill, whole):
+    """Plain and capped training steps on a workspace built with slopes leave the next biased step as it was, bit for bit."""
+    plan = fcp.fcp_plan_blocks(lens, 128, 1, 2)
+    flags = BASE | spill | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0)
+    kinds = {"bias": dict(slopes=[0.5, 0.1]), "plain": {}, "cap": dict(softcap=20.0), "both": dict(softcap=5.0, slopes=[0.5, 0.1])}
+    runs = {name: Run(plan, 2, 1, d, 128, flags, seed=1, **kw) for name, kw in kinds.items()}
+    want = {}
+    for name, run in runs.items():
+        run.step()
+        want[name] = run.outputs()
+        run.ws_ptr = runs["bias"].ws_ptr
+    for name in ("bias", "plain", "bias", "cap", "both", "plain", "cap", "bias", "both"):
+        run = runs[name]
+        for x in (run.o, run.lse, run.dq, run.dk, run.dv):
+            x.fill_(float("nan"))
+        run.step()
+        for out, x in run.outputs().items():
+            assert np.array_equal(x, want[name][out]), (name, out)
