@@ -8,6 +8,8 @@
 #include <cstdio>
 #include <cstring>
 #include <functional>
+#include <iterator>
+#include <map>
 #include <mutex>
 #include <numeric>
 #include <queue>
@@ -741,52 +743,54 @@ void choose_split(const fcp_problem* p, bool forward_only, WsLayout* L) {
   L->chosen = !two_fwd && !two_dq;
 }
 
-// Layouts validated by fcp_queue_build, keyed by the workspace they were built into.  A launch on that
+// Layouts validated by fcp_queue_build, by the workspace they were built into.  A launch on that
 // workspace with the same descriptor scalars reuses the layout instead of walking every table again: the
 // kernels read the device copy of the tables that fcp_queue_build made, so the host tables matter to a
 // launch only through their counts.  A workspace the registry does not know (or a descriptor that differs)
 // takes the full validation path.  Scores are not part of the key: a workspace built with slopes serves all kinds, each by
-// the layout that it was built with; one built without them has none to read.
+// the layout that it was built with; one built without them has none to read, and too little room for a layout that has them.
+// An entry stays until something is built over its memory, so there are never more than workspaces fit into the devices' memory.
 namespace {
 struct LayoutKey {
-  const void* workspace;
   int32_t v[11];
-  bool operator==(const LayoutKey& o) const { return workspace == o.workspace && std::memcmp(v, o.v, sizeof(v)) == 0; }
+  bool operator==(const LayoutKey& o) const { return std::memcmp(v, o.v, sizeof(v)) == 0; }
 };
-LayoutKey make_key(const fcp_problem* p, const void* ws) {
-  return LayoutKey{ws, {p->n_q_heads, p->n_kv_heads, p->head_dim, p->block_size, p->flags & (FCP_FLAG_DIRECT_SINGLE | FCP_FLAG_BWD_SPILL_DS | FCP_FLAG_WHOLE_ITEMS),
-                        p->n_kv_blocks, p->n_q_blocks, p->n_pairs, p->n_slots, p->n_slot_rows, p->n_segments}};
+LayoutKey make_key(const fcp_problem* p) {
+  return LayoutKey{{p->n_q_heads, p->n_kv_heads, p->head_dim, p->block_size, p->flags & (FCP_FLAG_DIRECT_SINGLE | FCP_FLAG_BWD_SPILL_DS | FCP_FLAG_WHOLE_ITEMS),
+                    p->n_kv_blocks, p->n_q_blocks, p->n_pairs, p->n_slots, p->n_slot_rows, p->n_segments}};
 }
-constexpr int kLayoutCacheSize = 32;
-std::mutex g_layout_mutex;
-std::pair<LayoutKey, WsLayout> g_layout_cache[kLayoutCacheSize];
-int g_layout_count = 0, g_layout_next = 0;
+struct Built { LayoutKey key; WsLayout layout; };
+std::mutex g_built_mutex;
+std::map<uintptr_t, Built> g_built;
 }  // namespace
 
+void forget_layouts(const void* workspace, size_t bytes) {
+  const uintptr_t at = (uintptr_t)workspace;
+  std::lock_guard<std::mutex> lock(g_built_mutex);
+  // entries do not overlap: of those that begin in front, only the last can reach into it
+  auto it = g_built.lower_bound(at);
+  if (it != g_built.begin() && std::prev(it)->first + std::prev(it)->second.layout.total > at) --it;
+  while (it != g_built.end() && it->first < at + bytes) it = g_built.erase(it);
+}
+
 void remember_layout(const fcp_problem* p, const void* workspace, const WsLayout& L) {
-  const LayoutKey key = make_key(p, workspace);
-  std::lock_guard<std::mutex> lock(g_layout_mutex);
-  for (int i = 0; i < g_layout_count; i++)
-    if (g_layout_cache[i].first.workspace == workspace) { g_layout_cache[i] = {key, L}; return; }
-  g_layout_cache[g_layout_next] = {key, L};
-  g_layout_next = (g_layout_next + 1) % kLayoutCacheSize;
-  g_layout_count = std::min(g_layout_count + 1, kLayoutCacheSize);
+  std::lock_guard<std::mutex> lock(g_built_mutex);
+  g_built[(uintptr_t)workspace] = Built{make_key(p), L};
 }
 
 int layout_for(const fcp_problem* p, const void* workspace, WsLayout* L) {
+  bool built_here = false;       // something is
   if (p && workspace && p->softmax_scale >= 0.0f && softcap_ok(p)) {
-    const LayoutKey key = make_key(p, workspace);
-    std::lock_guard<std::mutex> lock(g_layout_mutex);
-    for (int i = 0; i < g_layout_count; i++) {
-      if (g_layout_cache[i].first.workspace == workspace && has_bias(p) && !g_layout_cache[i].second.bias) {
-        set_error("scores: the workspace was built without slopes"); return FCP_ERR_INVALID_ARG;
-      }
-      if (g_layout_cache[i].first == key) { *L = g_layout_cache[i].second; return FCP_OK; }
-    }
+    std::lock_guard<std::mutex> lock(g_built_mutex);
+    const auto it = g_built.find((uintptr_t)workspace);
+    built_here = it != g_built.end();
+    if (built_here && has_bias(p) && !it->second.layout.bias) { set_error("scores: the workspace was built without slopes"); return FCP_ERR_INVALID_ARG; }
+    if (built_here && it->second.key == make_key(p)) { *L = it->second.layout; return FCP_OK; }
   }
   try {
     int rc = validate_problem(p);
     if (rc) return rc;
+    if (workspace && has_bias(p) && !built_here) { set_error("scores: nothing was built with slopes into this workspace"); return FCP_ERR_INVALID_ARG; }
     rc = compute_layout(p, false, L);
     if (rc == FCP_OK) choose_split(p, false, L);
     return rc;
@@ -1385,6 +1389,7 @@ extern "C" int fcp_queue_build(const fcp_problem* p, void* workspace, size_t wor
   std::vector<unsigned char> host;
   rc = build_queue_image(p, x, L, false, &host);
   if (rc) return rc;
+  forget_layouts(workspace, L.total);
   hipError_t e = hipMemcpyAsync(workspace, host.data(), host.size(), hipMemcpyHostToDevice, (hipStream_t)stream);
   if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)stream);
   if (e != hipSuccess) { set_error("fcp_queue_build: %s", hipGetErrorString(e)); return FCP_ERR_HIP; }

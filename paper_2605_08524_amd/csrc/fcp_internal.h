@@ -132,6 +132,7 @@ void choose_split(const fcp_problem* p, bool forward_only, WsLayout* L);    // h
 // the layout of a problem on a workspace: from the registry that fcp_queue_build fills, else validated and computed
 int layout_for(const fcp_problem* p, const void* workspace, WsLayout* L);   // host
 void remember_layout(const fcp_problem* p, const void* workspace, const WsLayout& L);
+void forget_layouts(const void* workspace, size_t bytes);      // of everything built into this memory
 inline bool has_softcap(const fcp_problem* p) { return (p->flags & FCP_FLAG_SCORES) && p->scores && p->scores->softcap > 0.f; }
 inline bool has_bias(const fcp_problem* p) { return (p->flags & FCP_FLAG_SCORES) && p->scores && p->scores->slopes; }
 // what limits fcp_block_attn_fwd_static: 1 KB, 16 bytes per pair and 72 per forward item of the plan's query blocks as given

@@ -505,3 +505,30 @@ def test_layers_of_several_kinds_of_scores_take_turns_on_one_workspace(lens, d, 
         run.step()
         for out, x in run.outputs().items():
             assert np.array_equal(x, want[name][out]), (name, out)
+
+
+def test_a_workspace_is_known_for_as_long_as_nothing_is_built_over_it():
+    """Many workspaces of one process (a layer each): what the first ones were built with still stands after the last."""
+    plan = fcp.fcp_plan_blocks([300, 40], 128, 1, 2)
+    bias = dict(slopes=[0.5, 0.1])
+    plain, biased = (Run(plan, 2, 1, 64, 128, BASE, seed=1, **kw) for kw in ({}, bias))
+    biased.step()
+    want = biased.outputs()
+    others = [Run(plan, 2, 1, 64, 128, BASE, seed=1, **kw) for kw in ({}, bias) * 50]
+    with pytest.raises(fcp.FcpError) as e:                       # refused in front of any launch
+        fcp.fcp_block_attn_fwd_out(biased.p, plain.q, plain.k, plain.v, plain.o_part, plain.lse_part, plain.o, plain.lse, plain.ws_ptr)
+    assert e.value.code == -1 and "slopes" in str(e.value)
+    plain.ws_ptr = biased.ws_ptr
+    plain.step()
+    biased.step()
+    for name, x in biased.outputs().items():
+        assert np.array_equal(x, want[name]), name
+    # built over, from its start or from further in, the memory serves no slopes any more
+    small = fcp.Problem(fcp.fcp_plan_blocks([16], 128, 1, 0), 1, 1, 64, 128, 0.0, BASE)
+    assert fcp.fcp_workspace_bytes(small) <= fcp.fcp_workspace_bytes(biased.p) - 256
+    for run, at in ((others[1], 0), (others[3], 256)):
+        assert run.p.slopes is not None
+        fcp.fcp_queue_build(small, run.ws_ptr + at, fcp.fcp_workspace_bytes(small))
+        with pytest.raises(fcp.FcpError) as e:
+            run.step()
+        assert e.value.code == -1 and "slopes" in str(e.value)

@@ -215,3 +215,16 @@ print('fine')
 """ % os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and "fine" in r.stdout, (r.returncode, r.stderr[-500:])
+
+
+def test_slopes_need_a_workspace_that_was_built_with_them():
+    """A workspace that nothing was built into may have been built without slopes: too small for a layout that has them."""
+    p = _problem(slopes=[0.5, 0.25])
+    x = 4096        # never read: the call ends before
+    for call in (lambda: B.fcp_block_attn_fwd(p, x, x, x, x, x, x), lambda: B.fcp_block_attn_fwd_out(p, x, x, x, x, x, x, x, x),
+                 lambda: B.fcp_merge_partials(p, x, x, x, x, x), lambda: B.fcp_bwd_preprocess(p, x, x, x, x), lambda: B.fcp_block_attn_bwd(p, x, x, x, x, x, x, x, x, x, x),
+                 lambda: B.fcp_block_attn_bwd_dkdv(p, x, x, x, x, x, x, x), lambda: B.fcp_block_attn_bwd_dq(p, x, x, x, x, x, x),
+                 lambda: B.fcp_block_attn_bwd_dq_d(p, x, x, x, x, x, x, x, x)):
+        with pytest.raises(B.FcpError) as e:
+            call()
+        assert e.value.code == B.FCP_ERR_INVALID_ARG and "slopes" in str(e.value)
