@@ -248,7 +248,7 @@ def fcp_stage_tables(plan, stage):
 class Problem:
     """Owns the host tables of an fcp_problem and the ctypes struct pointing at them.
 
-    softcap, slopes, q_pos, kv_pos: the scores (fcp_scores); with a softcap or slopes FCP_FLAG_SCORES is set."""
+    softcap, slopes, q_pos, kv_pos: the scores (fcp_scores); with any of them FCP_FLAG_SCORES is set."""
 
     def __init__(self, plan, n_q_heads, n_kv_heads, head_dim, block_size, softmax_scale=0.0, flags=0, softcap=0.0, slopes=None, q_pos=None, kv_pos=None):
         self.kv_blocks = _i32(plan["kv_blocks"]).reshape(-1, 4)
@@ -257,7 +257,7 @@ class Problem:
         self.slots = _i32(plan["slots"]).reshape(-1, 4)
         self.n_slot_rows = int(plan["n_slot_rows"])
         self.segments = _i32(plan["segments"]).reshape(-1, 4) if "segments" in plan else np.zeros((0, 4), dtype=np.int32)
-        if softcap or slopes is not None:
+        if softcap or any(x is not None for x in (slopes, q_pos, kv_pos)):
             flags = int(flags) | FCP_FLAG_SCORES
         self.flags = int(flags)
         self.softcap = float(softcap)

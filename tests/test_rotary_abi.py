@@ -103,3 +103,16 @@ def test_row_positions_refusals():
     plan = dict(fcp.fcp_plan_blocks([200], 128, 0, 0), q_blocks=np.array([[0, 5, 0, 128], [0, 1, 128, 72]]))
     with pytest.raises(B.FcpError):
         fcp.fcp_row_positions(B.Problem(plan, 2, 1, 64, 128))
+
+
+def test_row_positions_of_plain_scores_at_given_positions():
+    """Positions alone, without a softcap or slopes: a cache with gaps for rotary positions."""
+    plan = fcp.fcp_plan_blocks([200], 128, 0, 0)
+    p = B.Problem(plan, 2, 1, 64, 128, q_pos=[1000, 7], kv_pos=[50, 2000])
+    q, kv = fcp.fcp_row_positions(p)
+    assert np.array_equal(q, list(range(1000, 1128)) + list(range(7, 79))) and np.array_equal(kv, list(range(50, 178)) + list(range(2000, 2072)))
+    assert B.fcp_workspace_bytes(p) == B.fcp_workspace_bytes(B.Problem(plan, 2, 1, 64, 128))       # scores stay plain
+    for kw in (dict(q_pos=[0, 128]), dict(kv_pos=[0, 128]), dict(q_pos=[0, -1], kv_pos=[0, 128])):
+        with pytest.raises(B.FcpError) as e:
+            fcp.fcp_row_positions(B.Problem(plan, 2, 1, 64, 128, **kw))
+        assert e.value.code == B.FCP_ERR_INVALID_ARG
