@@ -58,7 +58,7 @@ typedef struct {
  * Angles are those of `turn` at every position; sine and cosine are good to 2e-7.  Arithmetic is fp32.  The call keeps nothing and
  * allocates nothing; it may be captured into a graph (the frequencies then are those of the capture).
  * Errors: FCP_ERR_INVALID_ARG (NULL, counts, an axis out of range, a stride below a row, one tensor with two strides or types),
- * FCP_ERR_UNSUPPORTED (dimensions or alignments other than above).
+ * FCP_ERR_UNSUPPORTED (dimensions or alignments other than above; more than 2^24 - 1 groups of four rows, which is 67 million rows in one part).
  */
 int fcp_rotary_apply(const fcp_rotary* r, const fcp_rotary_part* parts, int32_t n_parts, int32_t inverse, void* stream);
 

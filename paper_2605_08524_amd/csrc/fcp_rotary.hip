@@ -23,6 +23,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kMaxPairs = FCP_ROTARY_MAX_DIM / 2;
 constexpr int kThreads = 256;
+constexpr int64_t kMaxGroups = ((int64_t)1 << 32) / kThreads - 1;     // a launch has fewer than 2^32 threads
 
 struct RotaryArgs {
   fcp_rotary_part part[FCP_ROTARY_MAX_PARTS];
@@ -179,7 +180,7 @@ extern "C" int fcp_rotary_apply(const fcp_rotary* r, const fcp_rotary_part* part
     n += ((int64_t)parts[i].n_rows + a.rows - 1) / a.rows;
     a.first_group[i + 1] = n;
   }
-  if (n > INT32_MAX) { set_error("fcp_rotary_apply: too many rows for one launch"); return FCP_ERR_UNSUPPORTED; }
+  if (n > kMaxGroups) { set_error("fcp_rotary_apply: too many rows for one launch (%lld groups of %d, at most %lld)", (long long)n, a.rows, (long long)kMaxGroups); return FCP_ERR_UNSUPPORTED; }
   void (*kern)(RotaryArgs) = r->interleaved ? rotary_kernel<true> : rotary_kernel<false>;
   hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(kThreads), a.rows * a.n_pairs * sizeof(f32x2), (hipStream_t)stream, a);
   const hipError_t e = hipGetLastError();

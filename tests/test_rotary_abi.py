@@ -116,3 +116,9 @@ def test_row_positions_of_plain_scores_at_given_positions():
         with pytest.raises(B.FcpError) as e:
             fcp.fcp_row_positions(B.Problem(plan, 2, 1, 64, 128, **kw))
         assert e.value.code == B.FCP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("rows,parts", [(2 ** 26 - 3, 1), (2 ** 31 - 1, 1), (2 ** 24 - 3, 4)])
+def test_rotary_refuses_more_rows_than_a_launch_holds(rows, parts):
+    """2^24 workgroups of 256 threads are one more than HIP takes.  Refused in front of the launch: the pointers are never read."""
+    assert _call({}, dict(n_rows=rows), parts) == B.FCP_ERR_UNSUPPORTED and "too many rows" in B.fcp_last_error()
