@@ -24,8 +24,8 @@ enum { FCP_ROTARY_MAX_AXES = 8, FCP_ROTARY_MAX_PARTS = 4, FCP_ROTARY_MAX_DIM = 2
  * fcp_rotary_turns -- frequencies as the kernel wants them, once per model (host).
  *
  * freq: host, [n], radians per position, |freq| <= 1e6 (FCP_ERR_INVALID_ARG otherwise).  turn: host, [n]: the fraction of a turn per
- * position, in units of 2^-64, off by one unit and by 2^-64 of the frequency.  A position times it, modulo 2^64, is the angle modulo one
- * turn, exactly: with |freq| up to 1 the angle is good to 2^-32 of a turn at any position.
+ * position, in units of 2^-64, off by at most 1 + |freq| / 4 of them.  A position times it, modulo 2^64, is the angle modulo one
+ * turn, off by |pos| (1 + |freq| / 4) 2^-64 turns: with |freq| up to 1 at most 2^-32 of a turn, with the largest 2^-15, at positions of 2^31.
  */
 int fcp_rotary_turns(const double* freq, int32_t n, uint64_t* turn);
 

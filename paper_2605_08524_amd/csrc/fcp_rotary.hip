@@ -3,8 +3,9 @@
 // Memory-bound: every element is read once and written once, 6 FLOP a pair.  A workgroup takes kRows rows of one tensor; it first works
 // out cos and sin of their angles, one per (row, pair), into LDS, where all heads of the row share them, and then streams the rows,
 // 16 dimensions (8 pairs) of a head a thread and step: two 16-byte accesses each way in bf16, 128-byte lines in whole.
-// Angles.  A position times a frequency in fp32 is off by 0.06 at position 10^6 (half a unit of 2^-4), so the frequency comes as a 64-bit fraction
-// of a turn and the product wraps modulo 2^64, that is modulo one turn: exact for every position, 2^-33 of a turn for the largest.
+// Angles.  A position times a frequency of 1 in fp32 is off by 0.03 at position 10^6 (half a unit of 2^-4), so the frequency comes as a 64-bit fraction
+// of a turn and the product wraps modulo 2^64, that is modulo one turn, exactly.  What is left is the fraction's own error times the position,
+// |pos| (1 + |freq| / 4) 2^-64 turns, and 2^-33 where the product is rounded to 32 bits.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -128,7 +129,7 @@ extern "C" int fcp_rotary_turns(const double* freq, int32_t n, uint64_t* turn) {
   if (n < 0 || (n > 0 && (!freq || !turn))) { set_error("fcp_rotary_turns: invalid argument"); return FCP_ERR_INVALID_ARG; }
   for (int p = 0; p < n; p++) {
     if (!(std::fabs(freq[p]) <= 1e6)) { set_error("fcp_rotary_turns: |freq[%d]| must be at most 1e6", p); return FCP_ERR_INVALID_ARG; }
-    // 64 bits of mantissa: off by 2^-64 of the frequency, and of a turn
+    // 64 bits of mantissa: the divisor and the quotient are off by half a unit each, 1.5 2^-64 freq / 2 pi at most; cutting the rest off is one more 2^-64
     const long double turns = (long double)freq[p] / 6.28318530717958647692528676655900577L;
     const long double fraction = turns - floorl(turns);
     turn[p] = fraction >= 1.0L ? 0 : (uint64_t)(fraction * 18446744073709551616.0L);

@@ -122,3 +122,22 @@ def test_row_positions_of_plain_scores_at_given_positions():
 def test_rotary_refuses_more_rows_than_a_launch_holds(rows, parts):
     """2^24 workgroups of 256 threads are one more than HIP takes.  Refused in front of the launch: the pointers are never read."""
     assert _call({}, dict(n_rows=rows), parts) == B.FCP_ERR_UNSUPPORTED and "too many rows" in B.fcp_last_error()
+
+
+def test_rotary_turns_are_as_good_as_stated():
+    """Off by at most 1 + |freq| / 4 units of 2^-64 turns, against 2 pi in integers (Machin's formula, 2^-300)."""
+    one = 1 << 300
+
+    def arctan_inverse(n):
+        total, term, k, sign = 0, one // n, 1, 1
+        while term:
+            total, term, k, sign = total + sign * (term // k), term // (n * n), k + 2, -sign
+        return total
+    two_pi = 8 * (4 * arctan_inverse(5) - arctan_inverse(239))
+    rng = np.random.default_rng(0)
+    freq = np.concatenate([10000.0 ** (-np.arange(64) / 64), 10.0 ** rng.uniform(-12, 6, 400) * rng.choice([-1, 1], 400), [1e6, -1e6, 2 * np.pi, np.pi]])
+    for f, t in zip(freq, fcp.fcp_rotary_turns(freq)):
+        num, den = float(f).as_integer_ratio()
+        want = (num * one << 128) // (den * two_pi)                     # units of 2^-128 turns
+        off = (((int(t) << 64) - want + (1 << 127)) % (1 << 128)) - (1 << 127)
+        assert abs(off) / 2.0 ** 64 <= 1 + abs(f) / 4, f
