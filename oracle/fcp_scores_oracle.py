@@ -3,7 +3,8 @@
     z = scale q.k;  y = cap tanh(z / cap) (cap > 0);  s = y - slope_h |pos_i - pos_j|;  softmax over the visible keys of a row
 
 and its gradient.  Beside every result stands a bound on what an implementation may be off that keeps P and dS as bf16 operands
-and everything else in fp32: a bf16 rounding is off by at most HALF = 2^-8 of the value, an exponent x in fp32 by 2^-22 |x| or so."""
+and everything else in fp32: a bf16 rounding is off by at most HALF = 2^-8 of the value, an exponent x in fp32 by 2^-22 |x| or so.
+Bounds are an element's own: keys that have no weight in a row loosen none of its."""
 from __future__ import annotations
 
 import numpy as np
@@ -64,29 +65,36 @@ def attention(q, k, v, see, dist, cap=0.0, slopes=None, scale=None, d_o=None, o_
             tot = p.sum(1)
             lse[:, h] = np.where(tot > 0, np.log(tot) + top, -np.inf)
             p = np.where(tot[:, None] > 0, p / np.where(tot > 0, tot, 1)[:, None], 0.0)
-        # what fp32 does to an exponent, as a relative error of P
-        ex = 2.0 ** -20 + 2.0 ** -21 * (np.where(see, big, 0).max(initial=0) + 2 * cap)
+        # What fp32 does to the exponent of an element, as a relative error of its P: sums and products of this size, the LSE that is taken off, and
+        # a bias that is formed along the 64 columns of a tile, 64 slopes from their first to their last.
+        fin = np.where(np.isfinite(lse[:, h]), lse[:, h], 0)
+        ex = 2.0 ** -20 + 2.0 ** -21 * (big + 2 * cap + np.abs(fin)[:, None]) + (2.0 ** -17 * float(np.float32(slopes[h])) if slopes is not None else 0.0)
+        r = HALF + ex
+        pr = p * r
         o[:, h] = p @ vh
-        # Every P_j V_j carries a rounding (1 + r_j), |r_j| <= h = HALF + ex.  Divided by the sum of P as it is, O is off by |sum P_j r_j V_j|
-        # <= h P|V|.  Divided by the sum of the rounded P it is sum P_j (1 + r_j) V_j / sum P_j (1 + r_j), off by
-        # |sum P_j r_j (V_j - O)| / |1 + sum P_j r_j| <= h / (1 - h) (P|V| + |O|), the larger one.
-        eo[:, h] = (HALF + ex) / (1 - HALF - ex) * (p @ np.abs(vh) + np.abs(o[:, h])) + (HALF * np.abs(o[:, h]) if o_bf16 else 0)
-        el[:, h] = ex + 2.0 ** -21 * np.abs(np.where(np.isfinite(lse[:, h]), lse[:, h], 0))
+        # Every P_j V_j carries a rounding (1 + r_j), |r_j| <= r.  Divided by the sum of P as it is, O is off by |sum P_j r_j V_j|
+        # <= (P r)|V|.  Divided by the sum of the rounded P it is sum P_j (1 + r_j) V_j / sum P_j (1 + r_j), off by
+        # |sum P_j r_j (V_j - O)| / |1 + sum P_j r_j| <= ((P r)|V| + sum(P r)|O|) / (1 - sum(P r)), the larger one.
+        all_r = pr.sum(1)[:, None]
+        eo[:, h] = (pr @ np.abs(vh) + all_r * np.abs(o[:, h])) / (1 - all_r) + (HALF * np.abs(o[:, h]) if o_bf16 else 0)
+        el[:, h] = (p * ex).sum(1) + 2.0 ** -21 * np.abs(fin)
         if d_o is None:
             continue
         do = d_o[:, h]
         dp, dsum = do @ vh.T, (do * o[:, h]).sum(1)
         f = (1 - t * t) * scale if cap else np.full_like(z, scale)
         ds = p * (dp - dsum[:, None]) * f
-        # D comes from the O that was stored; dP and D are sums in fp32
+        # P is formed anew, against the LSE that was stored; D comes from the O that was stored; dP and D are sums in fp32
+        r = r + el[:, h][:, None]
+        pr = p * r
         e_d = (np.abs(do) * eo[:, h]).sum(1)
-        e_ds = (HALF + ex) * np.abs(ds) + p * f * (e_d[:, None] + 2.0 ** -18 * (np.abs(do) @ np.abs(vh).T))
+        e_ds = r * np.abs(ds) + p * f * (e_d[:, None] + 2.0 ** -18 * (np.abs(do) @ np.abs(vh).T))
         if cap:
             e_ds += p * np.abs(dp - dsum[:, None]) * scale * 2.0 ** -20          # 1 - tanh^2 in absolute terms
         for name, val, err in (("dq", ds @ kh, e_ds @ np.abs(kh)),):
             g[name][0][:, h] += val
             g[name][1][:, h] += err
-        for name, val, err in (("dk", ds.T @ qh, e_ds.T @ np.abs(qh)), ("dv", p.T @ do, (HALF + ex) * (p.T @ np.abs(do)))):
+        for name, val, err in (("dk", ds.T @ qh, e_ds.T @ np.abs(qh)), ("dv", p.T @ do, pr.T @ np.abs(do))):
             g[name][0][:, h // group] += val
             g[name][1][:, h // group] += err
     out = {"o": (o, eo + 1e-7), "lse": (lse, el)}

@@ -72,3 +72,19 @@ def test_closed_forms():
     see[3] = False
     r = sorc.attention(q, k, v, see, dist, 3.0, (0.5, 0.5), d_o=do)
     assert np.all(r["o"][0][3] == 0) and np.all(np.isneginf(r["lse"][0][3])) and np.all(r["dq"][0][3] == 0)
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_keys_without_weight_loosen_no_bound(cap):
+    """Bounds of a row with far keys under a steep slope are those without them (to 1 %), and a bf16 half step of the outputs' terms or so."""
+    (q, k, v, do), see, dist = _inputs([40], 2, 1, 16, 7)
+    slopes = (40.0, 8.0)
+    near = see & (dist < 8)
+    far = dist + 1000 * (dist >= 8)
+    a, b = (sorc.attention(q, k, v, s, far, cap, slopes, 0.25, do) for s in (near, see))
+    for name in a:
+        assert np.abs(a[name][0] - b[name][0]).max() < 1e-12, name
+        assert (b[name][1] <= 1.01 * a[name][1]).all(), name
+    half = sorc.HALF
+    p_v = np.abs(v).repeat(2, 1)                                            # next to nothing but the own token is left
+    assert (b["o"][1] <= 1.1 * half * 2 * p_v + 2e-3).all() and (b["lse"][1] <= 64 * 40.0 * 2.0 ** -21).all()
