@@ -68,7 +68,9 @@ typedef struct { int32_t kv_blk, seq, tok_off, tok_len; } fcp_segment;
  *   both or neither.  NULL: a block's position is the number of tokens of its sequence in the kv_blocks before it, as in the tables of
  *   the planners here (FCP_ERR_INVALID_ARG if a query block is none of the kv_blocks, or a pair joins different sequences).
  *   The blocks of a DIAG pair are at one position (FCP_ERR_INVALID_ARG with slopes otherwise).  PACKED kinds go by the rows' places in
- *   their block either way. */
+ *   their block either way.
+ * However far a row's nearest key is: O is as good as for near ones.  The LSE is fp32, off by 2^-21 of its value; the backward, which forms
+ *   P from it, is off by as much, relatively, times |LSE| (gradients of rows with |LSE| beyond 2^14 lose bits, beyond 2^20 they mean nothing). */
 typedef struct { float softcap; const float* slopes; const int32_t* q_pos; const int32_t* kv_pos; } fcp_scores;
 
 enum {

@@ -393,15 +393,30 @@ __device__ __forceinline__ Item load_record(const Item* p) {
   return u.it;
 }
 
-// Distance of the nearest key that row `row` of an item's segment sees: 0 where a span holds the row's own token.
-__device__ __forceinline__ float nearest_key(const DevPair* spans, const int32_t* rels, const QItem& it, int row) {
-  int near = 0x7fffffff;
-  for (int i = 0; i < it.n_pairs; i++) {
+// Distance of the nearest key that an item's rows see: of the rows lo .. lo + 31 of its segment (wave-uniform), 0 where a span holds a row's own
+// token, and, with ROW, how much further away that of row `row` is.  The forward takes `wave` off every distance while it is an integer, and slope * wave
+// off the LSE at the end.  Bias and reference in fp32 would lose the scores of a share whose keys are all far: its exponents, differences of two
+// large numbers, are then off by 2^-24 of slope * distance, and P is infinite from 2^30 on.  Costs 0.2 to 0.9 % of the forward, scalar work a tile.
+struct Nearest { int wave; float row; };
+// A running maximum may start with keys much further away than the nearest.  Their biases end at 2^29 (log2 units; their P is 0 or becomes 0 then):
+// P is at most 2^32 at the first of them, half a unit of 2^29, and goes with the next rescaling.
+__device__ __forceinline__ int farthest(float slope_log2) { return (int)fminf(0x1p29f / __builtin_fabsf(slope_log2), 2e9f); }
+// Signed distance of a wave's first row from the first column of a span, less `near`.  (With a `near` all keys of a span are on one side of all rows.)
+__device__ __forceinline__ int less_near(int d, int near) { return d > 0 ? d - near : d + near; }
+template <bool ROW>
+__device__ __forceinline__ Nearest nearest_key(const DevPair* spans, const int32_t* rels, const QItem& it, int lo, int row) {
+  if (it.n_pairs <= 0 || it.diag_last >= 0) return {0, 0.f};
+  int wave = 0x7fffffff, own = 0x7fffffff;
+  for (int i = __builtin_amdgcn_readfirstlane(it.n_pairs) - 1; i >= 0; i--) {
     const DevPair sp = i ? load_record(spans + it.pair_begin + i) : it.first;
-    const int d = load_rel(rels + it.pair_begin + i) + row;
-    near = sp.kind != FCP_KIND_FULL ? 0 : min(near, max(max(d - (sp.kv_len - 1), -d), 0));
+    const int rel = __builtin_amdgcn_readfirstlane(load_rel(rels + it.pair_begin + i)), len = __builtin_amdgcn_readfirstlane(sp.kv_len);
+    if (__builtin_amdgcn_readfirstlane(sp.kind) != FCP_KIND_FULL) return {0, 0.f};
+    const int d = rel + __builtin_amdgcn_readfirstlane(lo);
+    wave = min(wave, max(d > 0 ? d - (len - 1) : -d - 31, 0));
+    if constexpr (ROW) own = min(own, max(max(rel + row - (len - 1), -(rel + row)), 0));
+    else if (wave == 0) break;
   }
-  return (float)(it.n_pairs > 0 ? near : 0);
+  return {__builtin_amdgcn_readfirstlane(wave), ROW ? (float)(own - wave) : 0.f};
 }
 
 // =====================================================================================
@@ -618,10 +633,13 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
     if constexpr (STATIC) {
       top = fminf(a.mod.cap_a, kStaticTop);
       m_run = a.mod.cap_a - top;
-      if constexpr (MOD & kBias) {
-        const float b = slope * nearest_key(a.spans, a.mod.rel, it, my_limit);
-        m_run += b; top -= b;
-      }
+    }
+    int near = 0, far = 0x7fffffff;   // kBias: taken off every distance, see nearest_key; where distances end
+    if constexpr (MOD & kBias) {
+      if constexpr (!STATIC) far = __builtin_amdgcn_readfirstlane(farthest(slope * to_log2));
+      const Nearest n = nearest_key<STATIC>(a.spans, a.mod.rel, it, wave_row_lo, my_limit);
+      near = n.wave;
+      if constexpr (STATIC) { m_run += slope * n.row; top -= slope * n.row; }
     }
     // STATIC: the exponentials of a tile start while the tile before it is still being added to O, so that every MFMA has an element's
     // worth of vector work beside it (42 cycles against its 32): elements 0-7 of tile i+1 run between the last MFMAs of V P of tile i.
@@ -656,9 +674,11 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
     uint32_t d_lim = 0, lim_last = 0;
     int left = 0, span = 0;           // tiles of the span in hand not yet described, less one; its number
     int d_word = 0;                   // 4 * (columns that need no mask - first column - 64) + kind: below zero needs a mask
-    int d_rel = 0;                    // kBias: position of the segment's first row less that of the tile's first column
+    int d_rel = 0;                    // kBias: position of the wave's first row less that of the tile's first column, and less `near`
     auto open_span = [&](const DevPair& sp) {
-      if constexpr (MOD & kBias) d_rel = load_rel(a.mod.rel + it.pair_begin + (back ? it.n_pairs - 1 - span : span));
+      if constexpr (MOD & kBias) {
+        d_rel = less_near(__builtin_amdgcn_readfirstlane(load_rel(a.mod.rel + it.pair_begin + (back ? it.n_pairs - 1 - span : span))) + wave_row_lo, near);
+      }
       // wave-uniform: readfirstlane says so to the compiler, which then keeps what follows in scalar registers
       const int kv_start = __builtin_amdgcn_readfirstlane(sp.kv_start), kv_len = __builtin_amdgcn_readfirstlane(sp.kv_len);
       const int kind = __builtin_amdgcn_readfirstlane(sp.kind), diag = __builtin_amdgcn_readfirstlane(sp.ext);
@@ -718,15 +738,16 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
     if (wave == 0 && short_item) items.request(lane);
     // prologue: tiles 0 and 1
     int word[3];                      // d_word of tiles i+1, i+2, i+3 (shift register)
-    int rels[3];                      // d_rel of the same
+    int rels[3];                      // d_rel of the same, within +-far
+    auto rel_now = [&]() { return (MOD & kBias) && !STATIC ? min(max(d_rel, -far), far) : d_rel; };
     if constexpr (MAY_BACK) {
       if (it.n_pairs > 0 && (it.n_pairs == 1 || !back)) open_span(it.first); else describe();
     } else {
       if (it.n_pairs > 0) open_span(it.first); else describe();
     }
-    issue(); word[0] = d_word; rels[0] = d_rel;
-    describe(); issue(); word[1] = d_word; rels[1] = d_rel;
-    describe(); word[2] = d_word; rels[2] = d_rel;     // tile 2, requested inside the first iteration
+    issue(); word[0] = d_word; rels[0] = rel_now();
+    describe(); issue(); word[1] = d_word; rels[1] = rel_now();
+    describe(); word[2] = d_word; rels[2] = rel_now();     // tile 2, requested inside the first iteration
     dma_wait();
     __syncthreads();
 
@@ -738,16 +759,15 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
 
     auto next_tile = [&]() {
       word[0] = word[1]; word[1] = word[2]; describe(); word[2] = d_word;
-      if constexpr (MOD & kBias) { rels[0] = rels[1]; rels[1] = rels[2]; rels[2] = d_rel; }
+      if constexpr (MOD & kBias) { rels[0] = rels[1]; rels[1] = rels[2]; rels[2] = rel_now(); }
     };
-    // kBias: signed distance of score e = 16 rt + r of tile i+1 (t = 0) or i+2: first_distance - column(e)
-    auto first_distance = [&](int t) { return (float)(__builtin_amdgcn_readfirstlane(rels[t]) + my_limit - 4 * g); };
+    // kBias: signed distance of score e = 16 rt + r of tile i+1 (t = 0) or i+2, less `near`: first_distance - column(e)
+    auto first_distance = [&](int t) { return (float)(__builtin_amdgcn_readfirstlane(rels[t]) + l32 - 4 * g); };
     auto column = [](int e) { return (float)(32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3)); };
     auto bias = [&](float d0, int e) { return slope * __builtin_fabsf(d0 - column(e)); };
     // A tile's keys lie on one side of the wave's rows but for those around the diagonal; under a causal mask nothing on the other side counts.
-    // (rels is compared, not added to: positions may be anything below 2^31)
-    auto behind = [&](int t) { return !(word[t] & 1) && rels[t] <= -(wave_row_lo + 31); };
-    auto both_sides = [&](int t) { return !(word[t] & 1) && rels[t] < kFwdTileN - 1 - wave_row_lo && rels[t] > -(wave_row_lo + 31); };
+    auto behind = [&](int t) { return !(word[t] & 1) && rels[t] <= -31; };
+    auto both_sides = [&](int t) { return !(word[t] & 1) && rels[t] < kFwdTileN - 1 && rels[t] > -31; };
     auto is_special = [&](int t) {
       if constexpr (MOD & kBias) { if (both_sides(t)) return true; }
       return __builtin_amdgcn_readfirstlane(word[t]) < 0;
@@ -1044,6 +1064,9 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
     const bool e_ok = e_row < (sub ? e.q_rows[1] : e.q_rows[0]);
     const int64_t e_q_row = (int64_t)((sub ? e.q_start[1] : e.q_start[0]) + e_row);
     const float l_tot = l_run + xor32(l_run);
+    float lse_s = m_run + __builtin_amdgcn_logf(l_tot);
+    if constexpr (MOD & kBias) lse_s += slope * to_log2 * (float)near;
+    lse_s = l_tot > 0.f ? lse_s * kLn2 : -INFINITY;
     float inv;
     if constexpr (STATIC) {
       const float n_tot = n_run + xor32(n_run);
@@ -1058,7 +1081,6 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
       const int64_t row = e_q_row;
       float* op = reinterpret_cast<float*>(a.o) + row * q_row_stride + (int64_t)e_head * D;
       float* lp = a.lse + row * a.n_q_heads + e_head;
-      const float lse_s = l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
       const float lse_o = *lp;
       const float m = fmaxf(lse_o, lse_s);
       const float w_o = lse_o == -INFINITY ? 0.f : __expf(lse_o - m);
@@ -1091,10 +1113,7 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) store_tile<false>(op + dt * 32, q_row_stride, rows, o[dt], inv, s_stage[wave], lane);
       }
-      if (g == 0 && e_ok) {
-        const float lse = l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
-        (to_final ? a.lse : a.lse_part)[(row0 + l32) * a.n_q_heads + e_head] = lse;
-      }
+      if (g == 0 && e_ok) (to_final ? a.lse : a.lse_part)[(row0 + l32) * a.n_q_heads + e_head] = lse_s;
     }
     // No barrier here: behind the last tile barrier no wave reads the ring, and the next item's loads start at once.
     item_idx = __builtin_amdgcn_readfirstlane(s_next);
@@ -1268,11 +1287,12 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
   SplitTiles tiles;
   tiles.init(a.spans, it, true, u.tile_off + u.rows, wave, lane);
   RelWindow rels;
-  float slope = 0.f, near = 0.f;
+  float slope = 0.f;
+  Nearest near = {0, 0.f};
+  int far = 0x7fffffff;
   if constexpr (MOD & kBias) {
     rels.init(a.mod.rel + it.pair_begin, it.n_pairs, lane);
     slope = -load_slope(a.mod.slopes + __builtin_amdgcn_readfirstlane(u.head)) * ((MOD & kCap) ? kLog2e : kLog2e / a.scale_log2);
-    if constexpr (STATIC) near = nearest_key(a.spans, a.mod.rel, it, u.tile_off + l32);
   }
   auto issue = [&](const uint16_t* base, uint32_t lds) {
     const int c0 = tiles.t * kSplitRows;
@@ -1288,6 +1308,10 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
     seg_lo = sg & 0xff; seg_hi = (sg >> 8) + 1;
     if (l32 >= u.rows) seg_hi = 0;
   }
+  if constexpr (MOD & kBias) {         // while the first tiles are on their way
+    near = nearest_key<STATIC>(a.spans, a.mod.rel, it, u.tile_off, my_limit);
+    if constexpr (!STATIC) far = __builtin_amdgcn_readfirstlane(farthest(slope * to_log2));
+  }
   loads_left<0>();
   __syncthreads();
 
@@ -1297,7 +1321,7 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
 #pragma unroll
     for (int r = 0; r < 16; r++) o[dt][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f, n_run = 0.f;
-  if constexpr (STATIC) m_run = a.mod.cap_a - fminf(a.mod.cap_a, kStaticTop) + slope * near;
+  if constexpr (STATIC) m_run = a.mod.cap_a - fminf(a.mod.cap_a, kStaticTop) + slope * near.row;
   bf16x8 qf[KC];
 #pragma unroll
   for (int kc = 0; kc < KC; kc++) qf[kc] = as_bf16x8(lds_read16(lds_addr(lds_q) + tile_off<D>(l32, 2 * kc + g)));
@@ -1310,7 +1334,10 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
     const DevPair cur = tiles.cur;
     const int c0 = tiles.t * kSplitRows;
     float d0 = 0.f;
-    if constexpr (MOD & kBias) d0 = (float)(rels.get(tiles.pair, lane) - c0 + my_limit - 4 * g);
+    if constexpr (MOD & kBias) {
+      const int d = less_near(rels.get(tiles.pair, lane) - c0 + u.tile_off, near.wave);
+      d0 = (float)((STATIC ? d : min(max(d, -far), far)) + l32 - 4 * g);      // as in fwd_kernel
+    }
     auto bias = [&](int r) { return slope * __builtin_fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))); };
     tiles.next(lane);
     const bool more = tiles.have;
@@ -1404,7 +1431,9 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
     }
     if (row >= u.rows) continue;
     const float div = STATIC ? n : l, inv = div > 0.f ? 1.0f / div : 0.f;
-    const float lse = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    float lse = m + __builtin_amdgcn_logf(l);
+    if constexpr (MOD & kBias) lse += slope * to_log2 * (float)near.wave;
+    lse = l > 0.f ? lse * kLn2 : -INFINITY;
     if (a.running) {
       // as in fwd_kernel
       const int64_t r = u.q_start + row;

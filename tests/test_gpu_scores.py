@@ -532,3 +532,67 @@ def test_a_workspace_is_known_for_as_long_as_nothing_is_built_over_it():
         with pytest.raises(fcp.FcpError) as e:
             run.step()
         assert e.value.code == -1 and "slopes" in str(e.value)
+
+
+def nearest_bound(run, see, dist):
+    """What the oracle says of a row whose nearest key is far: its distance taken off all of them leaves O as it is and the LSE more by slope * that.
+    The LSE's fp32 (this product, its sum and the change of base: seven roundings of half a step) is off by 2^-21 of its value."""
+    near = np.where(see, dist, np.iinfo(np.int64).max).min(1)
+    q, k, v, _ = (orc.bf16_to_f64(b) for b in run.bits)
+    want = sorc.attention(q, k, v, see, dist - near[:, None], run.p.softcap, run.p.slopes)
+    lse, el = want["lse"]
+    lse = lse - near[:, None] * run.p.slopes.astype(np.float64)[None]
+    return {"o": want["o"], "lse": (lse, el + 2.0 ** -21 * np.abs(lse))}
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("scores", ["bias", "both", "wide"])
+@pytest.mark.parametrize("far", [1003, 1000003, 20000001, 2 ** 30 + 1])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_whose_nearest_keys_are_far(d, far, scores, whole):
+    """A share without the keys around its rows: rows far behind their keys, rows far before them, rows between two runs of keys and next to
+    them, in blocks that follow each other and blocks that do not."""
+    kv = [100, 128, 70, 128, 128, 33, 1, 128]
+    kv_pos = [0, 100, 300, far + 3000, far + 3128, far + 3300, far + 90000, far + 3500]
+    q_len, q_pos = [70, 130, 1, 40, 40], [far + 3000 - 200, 2 * far if far < 2 ** 30 else far + 200000, 3 * (far // 4), far + 3400, far + 3340]
+    start = np.concatenate([[0], np.cumsum(kv)])
+    q_start = np.concatenate([[0], np.cumsum(q_len)])
+    see_blocks = [[0, 1, 2], [0, 1, 2, 6], [2, 0, 7, 3, 4, 5], [0, 6, 1], [7, 5]]
+    pairs = [(b, j, 0, b) for b, js in enumerate(see_blocks) for j in js]
+    slots, n = [], 0
+    for b, js in enumerate(see_blocks):
+        slots.append((b, n, len(js), q_start[b]))
+        n += len(js)
+    plan = dict(kv_blocks=[(0, i, start[i], n) for i, n in enumerate(kv)], q_blocks=[(0, 100 + b, q_start[b], n) for b, n in enumerate(q_len)],
+                pairs=pairs, slots=slots, n_slot_rows=q_start[-1])
+    slopes = [64.0, 8.0, 0.7, 2.0 ** -12]
+    run = Run(plan, 4, 2, d, 130, BASE | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0), backward=False, seed=21, q_scale=2.0, softcap=SCORES[scores][0], slopes=slopes,
+              q_pos=q_pos, kv_pos=kv_pos)
+    run.step()
+    kp = np.concatenate([p + np.arange(n) for p, n in zip(kv_pos, kv)])
+    qp = np.concatenate([p + np.arange(n) for p, n in zip(q_pos, q_len)])
+    see = np.zeros((len(qp), len(kp)), dtype=bool)
+    for b, js in enumerate(see_blocks):
+        for j in js:
+            see[q_start[b]:q_start[b + 1], start[j]:start[j + 1]] = True
+    want = nearest_bound(run, see, np.abs(qp[:, None] - kp[None]))
+    for name, x in run.outputs().items():
+        ref, bound = want[name]
+        assert np.isfinite(x).all(), name
+        worst = (np.abs(x - ref) / bound).max()
+        print(f"  {name}: worst {worst:.2f} of its bound", flush=True)
+        assert worst <= 1.0, (name, worst)
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("scores", ["bias", "both", "wide"])
+def test_far_keys_get_no_gradient_from_rows_that_have_near_ones(scores, whole):
+    """A share of keys that are all far, its backward given the LSE of rows whose near keys are elsewhere: P is 0 and so is every gradient."""
+    plan = dict(kv_blocks=[(0, 0, 0, 100), (0, 1, 100, 128)], q_blocks=[(0, 9, 0, 90)], pairs=[(0, 0, 0, 0), (0, 1, 0, 0)], slots=[(0, 0, 2, 0)], n_slot_rows=90)
+    run = Run(plan, 4, 2, 64, 128, BASE | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0), seed=22, softcap=SCORES[scores][0], slopes=[64.0, 8.0, 0.7, 0.01],
+              q_pos=[2 ** 31 - 91], kv_pos=[0, 100])
+    run.o.normal_()
+    run.lse.normal_()
+    fcp.fcp_block_attn_bwd(run.p, run.q, run.k, run.v, run.o, run.lse, run.d_o, run.dq, run.dk, run.dv, run.ws_ptr)
+    for name, x in run.outputs().items():
+        assert name in ("o", "lse") or not x.any(), name
