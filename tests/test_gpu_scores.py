@@ -596,3 +596,57 @@ def test_far_keys_get_no_gradient_from_rows_that_have_near_ones(scores, whole):
     fcp.fcp_block_attn_bwd(run.p, run.q, run.k, run.v, run.o, run.lse, run.d_o, run.dq, run.dk, run.dv, run.ws_ptr)
     for name, x in run.outputs().items():
         assert name in ("o", "lse") or not x.any(), name
+
+
+FORMS = dict(SCORES, plain=(0.0, False))
+
+
+def plan_of(geo):
+    lens, bs, mask, cut, c, hq, hkv, d, owned = GEOMETRY[geo]
+    plan = fcp.fcp_plan_blocks(lens, bs, int(mask == "causal"), c, owned) if cut is None else fcp.fcp_plan_blocks_cut(lens, cut, bs, int(mask == "prefix"), c, owned)
+    return plan, (hq, hkv, d, bs), geometry(sorc.layout(lens, bs, cut=cut, owned=owned), mask, cut)
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("geo", [g for g in GEOMETRY if GEOMETRY[g][3] is not None])
+def test_plain_scores_on_a_cut_plan(geo, whole):
+    plan, shape, seen = plan_of(geo)
+    for spill in (0, fcp.FCP_FLAG_BWD_SPILL_DS):
+        run = Run(plan, *shape, BASE | spill | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0), seed=31, q_scale=4.0)
+        run.step()
+        run.check(*seen)
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("scores", FORMS)
+@pytest.mark.parametrize("geo", ["ragged", "prefix_d128", "decode", "long_d128"])
+def test_a_bf16_o_goes_out_and_into_the_backward(geo, scores, whole):
+    """What inference hands out, and a training step that keeps no fp32 O: D is a sum over rounded values then, which the oracle's bound counts."""
+    plan, shape, seen = plan_of(geo)
+    cap, bias = FORMS[scores]
+    for spill in (0, fcp.FCP_FLAG_BWD_SPILL_DS):
+        flags = fcp.FCP_FLAG_DIRECT_SINGLE | fcp.FCP_FLAG_GRAD_BF16 | spill | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0)
+        run = Run(plan, *shape, flags, seed=32, q_scale=3.0, softcap=cap, slopes=alibi(shape[0]) if bias else None)
+        run.step()
+        run.check(*seen)
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("scores", FORMS)
+@pytest.mark.parametrize("o_flag", [0, fcp.FCP_FLAG_O_F32], ids=["bf16", "fp32"])
+def test_bf16_partials(o_flag, scores, whole):
+    """Each partial O is rounded once more: half a step of P|V|, which its slots share by their weights."""
+    cap, bias = FORMS[scores]
+    for geo in ("ragged_d128", "prefix", "decode_d128"):
+        plan, shape, (see, dist) = plan_of(geo)
+        flags = fcp.FCP_FLAG_DIRECT_SINGLE | fcp.FCP_FLAG_PART_BF16 | o_flag | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0)
+        run = Run(plan, *shape, flags, backward=False, seed=33, q_scale=2.0, softcap=cap, slopes=alibi(shape[0]) if bias else None)
+        run.o_part = torch.full_like(run.o_part, float("nan"), dtype=torch.bfloat16)
+        run.step()
+        q, k, v, _ = (orc.bf16_to_f64(b) for b in run.bits)
+        want = sorc.attention(q, k, v, see, dist, cap, run.p.slopes, o_bf16=not o_flag)
+        pv = sorc.attention(q, k, np.abs(v), see, dist, cap, run.p.slopes)["o"][0]
+        got = run.outputs()
+        # a partial is rounded with its errors of P in it (2 HALF P|V| at most), and the last rounding rounds this one's: 2 HALF^2 and HALF^2 more
+        assert (np.abs(got["o"] - want["o"][0]) <= want["o"][1] + (sorc.HALF + 3 * sorc.HALF ** 2) * pv).all()
+        assert (np.abs(got["lse"] - want["lse"][0]) <= want["lse"][1]).all()
