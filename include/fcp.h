@@ -70,11 +70,16 @@ typedef struct { int32_t kv_blk, seq, tok_off, tok_len; } fcp_segment;
  *   The blocks of a DIAG pair are at one position (FCP_ERR_INVALID_ARG with slopes otherwise).  PACKED kinds go by the rows' places in
  *   their block either way.
  * However far a row's nearest key is: O is as good as for near ones.  The LSE is fp32, off by 2^-21 of its value; the backward, which forms
- *   P from it, is off by as much, relatively, times |LSE| (gradients of rows with |LSE| beyond 2^14 lose bits, beyond 2^20 they mean nothing). */
+ *   P from it, is off by as much, relatively, times |LSE| (gradients of rows with |LSE| beyond 2^14 lose bits, beyond 2^20 they mean nothing).
+ * With a softcap up to 60 the forward takes its exponentials against a fixed reference instead of the row maximum, up to 2^72: the sum of |v| over the
+ *   keys of a row has to stay below 2^55, and where all scores of a row are within a few units of -softcap, a |v| below 2^-24 may count as 0.  O is
+ *   then 2^-8 of P|V| off where, with a row maximum, the largest P is exact (2-norm against 64 bits: 0.0021 with, 0.0019 without a softcap, of
+ *   which the rounding of O to bf16 is 0.0017). */
 typedef struct { float softcap; const float* slopes; const int32_t* q_pos; const int32_t* kv_pos; } fcp_scores;
 
 enum {
-  FCP_FLAG_O_F32 = 1,            /* the final O is fp32 instead of bf16 (the backward then reads fp32 O) */
+  FCP_FLAG_O_F32 = 1,            /* the final O is fp32 instead of bf16 (the backward then reads fp32 O).  For training: D = rowsum(dO o O) of a bf16 O
+                                    makes dQ and dK 0.0026 to 0.0031 off (2-norm against 64 bits, bf16 gradients), of an fp32 O 0.0024 to 0.0025 */
   FCP_FLAG_PART_BF16 = 4,        /* the partial O buffer (o_part) holds bf16 instead of fp32: half the memory and half the
                                     traffic of the partials; LSE partials stay fp32.  Set it for every call on a problem.
                                     A final O merged from bf16 partials carries bf16 rounding whatever its own dtype:
@@ -264,6 +269,7 @@ int fcp_queue_build(const fcp_problem* p, void* workspace, size_t workspace_byte
  *
  * Paper: section "Attention Computation" (O = Softmax(Q K^T / sqrt(D), mask) V) restricted to
  * the KV blocks of one stage; per-row log-sum-exp kept so that stages can be reduced later.
+ * P is rounded to bf16 where it is multiplied by V (half a step, 2^-8 of each); scores, sums, LSE and O are fp32 until they are written.
  * For slot s of query block b, rows r < tok_len(b):
  *   o_part [row_start(s) + r, h, :] = softmax over the slot's visible keys (normalised)
  *   lse_part[row_start(s) + r, h]   = ln sum exp(scale * q.k) over those keys
@@ -329,6 +335,7 @@ int fcp_merge_partials(const fcp_problem* p, const void* o_part, const float* ls
  * final LSE: D = rowsum(dO o O); P = exp(scale q.k - LSE); dV += P^T dO; dP = dO V^T;
  * dS = P o (dP - D); dQ += scale dS K; dK += scale dS^T Q; dK/dV are summed over the query
  * heads of a KV head and hold only the owned query rows' contribution.
+ * P and dS are rounded to bf16 where they are multiplied by dO, Q and K (and where the spill flag keeps dS); dP, D and all sums are fp32.
  * o: final O as written by fcp_merge_partials (dtype per flags); lse: final LSE; d_o bf16.
  * dq [T_q,Hq,d], dk, dv [T_kv,Hkv,d]: device fp32, or bf16 with FCP_FLAG_GRAD_BF16 (the fp32 sums are
  * rounded to nearest-even once, in the kernel that holds them: no cast pass); fully overwritten; every

@@ -529,6 +529,8 @@ namespace {
 // other) and split (fwd_split_kernel, bwd_split_kernel).  Forward and dQ: least-squares fits to 1300 to 1600 random problems a kernel and head
 // size, each run in both forms: 1 to 60 sequences, whole ones and only their last blocks, 1 to 128 heads, chains of 1 to 360 tiles.  Root mean square
 // error 8 to 12 % (whole) and 11 to 15 % (split).  dK/dV: fits to 58 shapes, which chose well on 2838 such problems too.
+// Modified scores go by the same fits: of 52 random launches that are split with a softcap and a bias the slowest takes 0.92 of what it takes whole
+// (geometric mean 0.49; plain scores 1.05 and 0.53), of 57 backward ones 0.77 (0.42; 0.83 and 0.48).
 // whole:  the start, and an end: dK/dV the longest item or the mean load and a time per item; forward and dQ every item on the compute unit
 //         that is free first.  An item in which at most half of the waves have rows walks its tiles faster.
 // split:  a start, the work, a time per workgroup (unit: 8, dK/dV 4) and the longest chain, which is an eighth; workgroups past the rows of

@@ -105,7 +105,7 @@ struct WsLayout {
   bool joint_bwd;   // fcp_block_attn_bwd runs split dQ and dK/dV in one launch
   SplitUnits fwd_units, dq_units;
   int split_kv_units;
-  bool bias;        // scores have a distance bias: the sections from off_slopes to off_span_rel are there
+  bool bias;        // built with slopes: off_slopes, off_span_rel, off_pair_rel and off_dep_rel have sections (else they are empty)
   int64_t n_ds_frags;   // fragments of the dS spill buffer, sinks and one fragment of slack included (0 without the flag)
   size_t off_pairs, off_spans, off_fwd_items, off_q_seg, off_bwd_deps, off_bwd_items, off_merge_items, off_slot_rh, off_dq_items, off_slopes, off_pair_rel, off_dep_rel, off_span_rel, off_dls, off_lse2, off_ds, total;
 };

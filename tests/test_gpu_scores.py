@@ -650,3 +650,21 @@ def test_bf16_partials(o_flag, scores, whole):
         # a partial is rounded with its errors of P in it (2 HALF P|V| at most), and the last rounding rounds this one's: 2 HALF^2 and HALF^2 more
         assert (np.abs(got["o"] - want["o"][0]) <= want["o"][1] + (sorc.HALF + 3 * sorc.HALF ** 2) * pv).all()
         assert (np.abs(got["lse"] - want["lse"][0]) <= want["lse"][1]).all()
+
+
+@pytest.mark.parametrize("whole", [False, True], ids=["split", "whole"])
+@pytest.mark.parametrize("cap", [20.0, 50.0, 60.3])
+def test_values_up_to_the_stated_sum(cap, whole):
+    """|v| of a row's keys summing up to 2^55, under scores at +softcap, at -softcap and in between."""
+    lens, bs = [300, 65], 128
+    plan = fcp.fcp_plan_blocks(lens, bs, 0, 1)
+    run = Run(plan, 2, 1, 64, bs, BASE | (fcp.FCP_FLAG_WHOLE_ITEMS if whole else 0), backward=False, seed=23, softcap=cap)
+    q, k, v = (workloads.bf16_to_f32(b) for b in run.bits[:3])
+    k[..., 0] = 64.0
+    q[0::3, :, 0], q[1::3, :, 0], q[2::3, :, 0] = -64.0, 64.0, 0.0
+    v *= np.float32(2.0 ** 55 / np.abs(v).sum(0).max() * 0.99)
+    for i, x in enumerate((q, k, v)):
+        run.bits[i] = workloads.bf16_bits(x)
+    run.q, run.k, run.v = (bits_to_dev(b) for b in run.bits[:3])
+    run.step()
+    run.check(*geometry(sorc.layout(lens, bs), "full"))
