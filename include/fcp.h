@@ -69,8 +69,9 @@ typedef struct { int32_t kv_blk, seq, tok_off, tok_len; } fcp_segment;
  *   the planners here (FCP_ERR_INVALID_ARG if a query block is none of the kv_blocks, or a pair joins different sequences).
  *   The blocks of a DIAG pair are at one position (FCP_ERR_INVALID_ARG with slopes otherwise).  PACKED kinds go by the rows' places in
  *   their block either way.
- * However far a row's nearest key is: O is as good as for near ones.  The LSE is fp32, off by 2^-21 of its value; the backward, which forms
- *   P from it, is off by as much, relatively, times |LSE| (gradients of rows with |LSE| beyond 2^14 lose bits, beyond 2^20 they mean nothing).
+ * However far the nearest key of a row in a slot is: the slot's O is as good as for near ones.  Its LSE is fp32, off by 2^-21 |LSE| at most, and so,
+ *   relatively, is what is formed from LSEs: the weights of several slots, and the P of the backward.  Beyond |LSE| = 2^14 they lose bits, beyond 2^20
+ *   they mean nothing, unless the row also has keys that are near (far ones then weigh 0, as they should).
  * With a softcap up to 60 the forward takes its exponentials against a fixed reference instead of the row maximum, up to 2^72: the sum of |v| over the
  *   keys of a row has to stay below 2^55, and where all scores of a row are within a few units of -softcap, a |v| below 2^-24 may count as 0.  O is
  *   then 2^-8 of P|V| off where, with a row maximum, the largest P is exact (2-norm against 64 bits: 0.0021 with, 0.0019 without a softcap, of

@@ -399,7 +399,7 @@ __device__ __forceinline__ Item load_record(const Item* p) {
 // Distance of the nearest key that an item's rows see: of the rows lo .. lo + 31 of its segment (wave-uniform), 0 where a span holds a row's own
 // token, and, with ROW, how much further away that of row `row` is.  The forward takes `wave` off every distance while it is an integer, and slope * wave
 // off the LSE at the end.  Bias and reference in fp32 would lose the scores of a share whose keys are all far: its exponents, differences of two
-// large numbers, are then off by 2^-24 of slope * distance, and P is infinite from 2^30 on.  Costs 0.2 to 0.9 % of the forward, scalar work a tile.
+// large numbers, are then off by 2^-24 of slope * distance, and P is infinite from 2^30 on.  Costs the biased forward up to 1 %, scalar work a tile.
 struct Nearest { int wave; float row; };
 // A running maximum may start with keys much further away than the nearest.  Their biases end at 2^29 (log2 units; their P is 0 or becomes 0 then):
 // P is at most 2^32 at the first of them, half a unit of 2^29, and goes with the next rescaling.
@@ -1067,9 +1067,10 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
     const bool e_ok = e_row < (sub ? e.q_rows[1] : e.q_rows[0]);
     const int64_t e_q_row = (int64_t)((sub ? e.q_start[1] : e.q_start[0]) + e_row);
     const float l_tot = l_run + xor32(l_run);
-    float lse_s = m_run + __builtin_amdgcn_logf(l_tot);
-    if constexpr (MOD & kBias) lse_s += slope * to_log2 * (float)near;
-    lse_s = l_tot > 0.f ? lse_s * kLn2 : -INFINITY;
+    auto slot_lse = [&]() {
+      if constexpr (MOD & kBias) return l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot) + slope * to_log2 * (float)near) * kLn2 : -INFINITY;
+      else return l_tot > 0.f ? (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
+    };
     float inv;
     if constexpr (STATIC) {
       const float n_tot = n_run + xor32(n_run);
@@ -1084,6 +1085,7 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
       const int64_t row = e_q_row;
       float* op = reinterpret_cast<float*>(a.o) + row * q_row_stride + (int64_t)e_head * D;
       float* lp = a.lse + row * a.n_q_heads + e_head;
+      const float lse_s = slot_lse();
       const float lse_o = *lp;
       const float m = fmaxf(lse_o, lse_s);
       const float w_o = lse_o == -INFINITY ? 0.f : __expf(lse_o - m);
@@ -1116,7 +1118,10 @@ __global__ void __launch_bounds__(512, 2) fwd_kernel(FwdArgs a) {
 #pragma unroll
         for (int dt = 0; dt < DT; dt++) store_tile<false>(op + dt * 32, q_row_stride, rows, o[dt], inv, s_stage[wave], lane);
       }
-      if (g == 0 && e_ok) (to_final ? a.lse : a.lse_part)[(row0 + l32) * a.n_q_heads + e_head] = lse_s;
+      if (g == 0 && e_ok) {
+        const float lse = slot_lse();
+        (to_final ? a.lse : a.lse_part)[(row0 + l32) * a.n_q_heads + e_head] = lse;
+      }
     }
     // No barrier here: behind the last tile barrier no wave reads the ring, and the next item's loads start at once.
     item_idx = __builtin_amdgcn_readfirstlane(s_next);
@@ -1434,9 +1439,8 @@ __global__ void __launch_bounds__(64 * kSplitWaves, D == 64 ? 4 : 2) fwd_split_k
     }
     if (row >= u.rows) continue;
     const float div = STATIC ? n : l, inv = div > 0.f ? 1.0f / div : 0.f;
-    float lse = m + __builtin_amdgcn_logf(l);
-    if constexpr (MOD & kBias) lse += slope * to_log2 * (float)near.wave;
-    lse = l > 0.f ? lse * kLn2 : -INFINITY;
+    float lse = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if constexpr (MOD & kBias) lse = l > 0.f ? (m + __builtin_amdgcn_logf(l) + slope * to_log2 * (float)near.wave) * kLn2 : -INFINITY;
     if (a.running) {
       // as in fwd_kernel
       const int64_t r = u.q_start + row;
